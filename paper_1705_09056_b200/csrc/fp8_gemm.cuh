@@ -27,11 +27,15 @@
 //   epilogue      (8) tcgen05.ld, bias, ReLU, rounding; a warp turns its 32 rows round in 4 KB of shared memory and writes
 //                 whole 128-byte lines
 // The tensor core truncates when it adds to an fp32 accumulator.  Where that can be seen in the result (fp32, or 8 bits,
-// where a value next to a tie would round the other way; g.hand = kSegment) the accumulator is handed over every 16 MMAs
-// and added up by the epilogue warps in registers, rounding to nearest; otherwise once per tile.  The epilogue takes an
-// accumulator into registers and frees it before it does anything else, so that even a single 256-column one (two leave
-// no room for the scales) keeps the tensor core waiting for a few hundred cycles only.  The registers come from the
-// other warps (setmaxnreg).
+// where a value next to a tie rounds the other way) the accumulator is handed over every 16 MMAs (g.hand = kSegment) and
+// added up by the epilogue warps in registers, rounding to nearest; otherwise once per tile.  Results in 8 bits from tiles
+// of 128 columns are handed over every 8 MMAs (kFineHand), which brings their sums from 1.06-1.25 times the error of plain
+// fp32 sums to 0.96-1.20 (32 nodes 32x784x1024 over six seeds) and costs 39.0 -> 40.5 us there, 473.6 -> 480.8 us on 112 nodes
+// 64x2048x2048, three accumulators in turn (40.9 and 484 us with two).  A tile of 256 columns has one accumulator and waits
+// at each hand-over (weights and product of 4 nodes 4096x4096x4096: 411 us every 16 MMAs, 521 every 8), so it keeps to 16.
+// The epilogue takes an accumulator into registers and frees it before it does anything else, so that even a single
+// 256-column one (two leave no room for the scales) keeps the tensor core waiting for a few hundred cycles only.  The
+// registers come from the other warps (setmaxnreg).
 // Measured: forward with a checkpoint out, 112 nodes 64 x 2048 x 2048: 92 us, 5.1 TB/s of 8-bit weights (the last round of
 // tiles is a tenth full); weight gradient of the same layer: 382 us from single CTAs, 4.9 TB/s of stores, held back by its
 // operand loads (335 us without them); forward, 4 nodes 4096 x 4096 x 4096: 225 us from single CTAs, 2.4 PFLOP/s.
@@ -60,7 +64,8 @@ constexpr int kTileM = 128;
 constexpr int kEpiWarps = 8;
 constexpr uint32_t kStageOut = 4096;                 // shared memory per epilogue warp
 constexpr uint32_t kSmemLimit = 232448;              // 227 KB per CTA
-constexpr int kSegment = 4;                          // k-blocks per scale word, and per promoted accumulator
+constexpr int kSegment = 4;                          // k-blocks per scale word, and per accumulator handed over
+constexpr int kFineHand = 2;                         // k-blocks per accumulator handed over where the result is rounded to 8 bits
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kScaleCol = 256, kScaleSet = 16;  // scale columns of a segment: 4 for A, up to 8 for B
 constexpr int kScaleSets = 4;
@@ -97,7 +102,11 @@ template <int MODE, int BN, bool PAIR> struct Shape {
     static constexpr int KPS = BN >= 256 ? 1 : BN == 128 ? 2 : 4;  // k-blocks per stage
     static constexpr int HALVES = BN >= 64 ? 2 : 1;                // column halves, four warps each
     static constexpr int COLS = BN / HALVES;                       // columns of a row one epilogue thread holds
-    static constexpr int ACCS = SCALED && BN == 256 ? 1 : 2;       // accumulators in tensor memory
+    // accumulators in tensor memory: one after the other from column 0, the third of 128 columns behind the scales
+    static constexpr int ACCS = SCALED && BN == 256 ? 1 : SCALED && BN == 128 ? 3 : 2;
+    static __device__ __forceinline__ uint32_t acc_col(uint32_t i) {
+        return i * (uint32_t)BN + (ACCS == 3 && i == 2 ? kScaleCol + kScaleSets * kScaleSet - 2 * (uint32_t)BN : 0u);
+    }
     static constexpr uint32_t MAXIMA = MODE == kForward && COLS == 64 ? 2048 : 0;   // [tile parity][half][128 rows]
     // alignment, output staging, barriers
     static constexpr uint32_t OUT = MODE == kWeight ? 0 : kStageOut;                // output staging of a warp
@@ -293,8 +302,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     uint64_t* full = reinterpret_cast<uint64_t*>(fixed_ptr + kEpiWarps * S::OUT + S::MAXIMA);
     uint64_t* empty = full + kMaxStages;
     uint64_t* acc_full = empty + kMaxStages;  // [2]
-    uint64_t* acc_empty = acc_full + 2;       // [2]
-    uint64_t* sf_full = acc_empty + 2;        // [kScaleSets]
+    uint64_t* acc_empty = acc_full + 3;       // [3]
+    uint64_t* sf_full = acc_empty + 3;        // [kScaleSets]
     uint64_t* sf_empty = sf_full + kScaleSets;
     uint64_t* max_full = sf_empty + kScaleSets;   // [4] both column halves of a lane quadrant have left their maxima
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(max_full + 4);
@@ -310,7 +319,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     }
     if (tid == 0) {
         for (int s = 0; s < g.stages; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 32 * 4 * S::HALVES * S::CTAS); }
+        for (int b = 0; b < 3; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 32 * 4 * S::HALVES * S::CTAS); }
         for (int b = 0; b < kScaleSets; ++b) { mbar_init(sf_full + b, 128 * S::CTAS); mbar_init(sf_empty + b, 1); }
         for (int b = 0; b < 4; ++b) mbar_init(max_full + b, 64);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -415,7 +424,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
                         tc::tc_fence_after();
                         uint64_t ad = a_base + s * stage_step, bd = b_base + s * stage_step;
                         const uint32_t sfa = tmem + kScaleCol + (seg_i % kScaleSets) * kScaleSet;
-                        const uint32_t d = tmem + ab0 * (uint32_t)BN;
+                        const uint32_t d = tmem + S::acc_col(ab0);
 #pragma unroll
                         for (int i = 0; i < KPS; ++i, ad += block_step, bd += block_step) {
                             const int kb = kb0 + i;
@@ -549,7 +558,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
                 const bool go = mbar_wait(acc_full + ab, (acc_i / ACCS) & 1u);
                 if (!__all_sync(0xffffffffu, go)) { ok = false; break; }  // tcgen05.ld needs the whole warp
                 tc::tc_fence_after();
-                const uint32_t acc = lanes + ab * (uint32_t)BN;
+                const uint32_t acc = lanes + S::acc_col(ab);
 #pragma unroll
                 for (int c = 0; c < COLS / 32; ++c) {
                     float v[32];

@@ -24,9 +24,9 @@ struct Operands {
     int64_t a_pitch, b_pitch;
 };
 
-// precise: hand accumulators over every 16 MMAs (see fp8_gemm.cuh).
+// fine: the result is rounded to 8 bits.  precise: to fp32, or fine (see fp8_gemm.cuh for how often sums are handed over).
 template <int MODE, int BN, bool PAIR>
-cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise) {
+cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool fine = false) {
     using S = Shape<MODE, BN, PAIR>;
     auto kernel = fp8_gemm_kernel<MODE, BN, PAIR>;
     const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
@@ -52,7 +52,7 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise) {
     if (!ok) return cudaErrorInvalidValue;
     const uint32_t stage_bytes = g.block_bytes * S::KPS;
     g.stages = std::min<int>(kMaxStages, (int)((kSmemLimit - S::FIXED) / stage_bytes));
-    g.hand = precise ? kSegment : INT32_MAX / 2;
+    g.hand = !precise ? INT32_MAX / 2 : fine && S::ACCS > 1 ? kFineHand : kSegment;
     g.m_tiles = (g.M + S::TM - 1) / S::TM;
     g.n_tiles = (g.N + BN - 1) / BN;
     const int64_t total = (int64_t)c->n * g.m_tiles * g.n_tiles;
@@ -75,15 +75,15 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise) {
 // last tiles of the weight gradient, where SMs become free one by one, and a pair needs two of them (the backward of those
 // nodes: level within the noise, 816-844 us either way).
 template <int MODE>
-cudaError_t launch_wide(dpsgd_ctx* c, const Operands& o, const Args& g, bool precise) {
+cudaError_t launch_wide(dpsgd_ctx* c, const Operands& o, const Args& g, bool precise, bool fine = false) {
     const int64_t sms = sm_count(c);
     const auto cost = [&](int rows, int cols) {                     // rounds over the SMs, times columns per CTA
         const int64_t tiles = (int64_t)c->n * ((g.M + rows - 1) / rows) * ((g.N + cols - 1) / cols) * (rows / kTileM);
         return (tiles + sms - 1) / sms * cols;
     };
     constexpr bool PAIR = MODE == kForward;
-    if (g.M > kTileM && cost(PAIR ? 2 * kTileM : kTileM, 256) <= cost(128, 128) * 1.3) return launch<MODE, 256, PAIR>(c, o, g, precise);
-    return launch<MODE, 128, false>(c, o, g, precise);
+    if (g.M > kTileM && cost(PAIR ? 2 * kTileM : kTileM, 256) <= cost(128, 128) * 1.3) return launch<MODE, 256, PAIR>(c, o, g, precise, fine);
+    return launch<MODE, 128, false>(c, o, g, precise, fine);
 }
 
 void set_out(Args& g, void* out, int dtype, int rows, int cols) {
@@ -116,7 +116,7 @@ cudaError_t launch_fp8_forward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* x
     // A checkpoint needs whole blocks of 128 columns in a tile.  Otherwise, few rows take narrower tiles so that every SM
     // has one; a tile costs about as much as 64 more columns before its first MMA (7 nodes 77x1001x1003: two rounds of 32
     // columns 19.4 us, one of 64 columns 18.4 us).
-    if (yq || tiles(128) >= sm_count(c)) return launch_wide<kForward>(c, o, g, precise);
+    if (yq || tiles(128) >= sm_count(c)) return launch_wide<kForward>(c, o, g, precise, yq != nullptr);
     const auto cost = [&](int bn) { return (tiles(bn) + sm_count(c) - 1) / sm_count(c) * (bn + 64); };
     return cost(64) <= cost(32) ? launch<kForward, 64, false>(c, o, g, precise) : launch<kForward, 32, false>(c, o, g, precise);
 }
