@@ -343,7 +343,11 @@ DPSGD_API dpsgd_status dpsgd_fp8_weights(dpsgd_ctx* ctx, int64_t w_off, int32_t 
  * A linear layer for all nodes at once (forward half of Algorithm 1 step 3), each node with its own weights:
  *   y[i][b][o] = act(sum_k x[i][b][k] w_i[o][k] + bias_i[o]),   act = ReLU when relu != 0, else the identity
  * x: checkpoint of [n][batch] rows of d_in;  w: from dpsgd_fp8_weights;  bias_i: fp32, columns [b_off, b_off + d_out) of
- * row i of the current X (b_off = -1: none).  The products of 8-bit numbers are exact and are added in fp32.
+ * row i of the current X (b_off = -1: none).  The products of 8-bit numbers are exact.  They are added in fp32 by the
+ * tensor core, which truncates: an accumulator takes at most 16 MMAs of 32 products (128 for a bf16 result without a
+ * checkpoint) before it is added to the others rounding to nearest.  With terms of one sign that loses at most 2^-19 of
+ * the sum (2^-17 for bf16; measured 2^-23.7 and less than bf16 shows).  The last bits of y depend on which outputs are
+ * asked for, and a checkpoint may differ from that of the exact sums by one E4M3 step next to a tie.
  *   y_dev       [n][batch][d_out] contiguous, fp32 or bf16; NULL: not wanted
  *   yq_dev/ye_dev  the output as a checkpoint (dpsgd_ckpt8_save of the fp32 result), formed in the same pass; NULL: not
  *               wanted.  At least one of the two forms must be given.

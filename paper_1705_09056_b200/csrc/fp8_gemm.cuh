@@ -28,7 +28,9 @@
 //                 whole 128-byte lines
 // The tensor core truncates when it adds to an fp32 accumulator.  Where that can be seen in the result (fp32, or 8 bits,
 // where a value next to a tie rounds the other way) the accumulator is handed over every 16 MMAs (g.hand = kSegment) and
-// added up by the epilogue warps in registers, rounding to nearest; otherwise once per tile.  Results in 8 bits from tiles
+// added up by the epilogue warps in registers, rounding to nearest.  bf16 results are handed over every 128 MMAs
+// (kCoarseHand, 4096 of the contraction): what that loses stays below 2^-16 of the sum of magnitudes, and products of up to
+// 4096 keep one accumulator per tile (every 64 MMAs cost 307 -> 318 us on 4 nodes 4096x4096x4096).  Results in 8 bits from tiles
 // of 128 columns are handed over every 8 MMAs (kFineHand), which brings their sums from 1.06-1.25 times the error of plain
 // fp32 sums to 0.96-1.20 (32 nodes 32x784x1024 over six seeds) and costs 39.0 -> 40.5 us there, 473.6 -> 480.8 us on 112 nodes
 // 64x2048x2048, three accumulators in turn (40.9 and 484 us with two).  A tile of 256 columns has one accumulator and waits
@@ -65,7 +67,7 @@ constexpr int kEpiWarps = 8;
 constexpr uint32_t kStageOut = 4096;                 // shared memory per epilogue warp
 constexpr uint32_t kSmemLimit = 232448;              // 227 KB per CTA
 constexpr int kSegment = 4;                          // k-blocks per scale word, and per accumulator handed over
-constexpr int kFineHand = 2;                         // k-blocks per accumulator handed over where the result is rounded to 8 bits
+constexpr int kFineHand = 2, kCoarseHand = 32;       // the same where the result is rounded to 8 bits, to bf16
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kScaleCol = 256, kScaleSet = 16;  // scale columns of a segment: 4 for A, up to 8 for B
 constexpr int kScaleSets = 4;

@@ -52,7 +52,7 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool f
     if (!ok) return cudaErrorInvalidValue;
     const uint32_t stage_bytes = g.block_bytes * S::KPS;
     g.stages = std::min<int>(kMaxStages, (int)((kSmemLimit - S::FIXED) / stage_bytes));
-    g.hand = !precise ? INT32_MAX / 2 : fine && S::ACCS > 1 ? kFineHand : kSegment;
+    g.hand = !precise ? kCoarseHand : fine && S::ACCS > 1 ? kFineHand : kSegment;
     g.m_tiles = (g.M + S::TM - 1) / S::TM;
     g.n_tiles = (g.N + BN - 1) / BN;
     const int64_t total = (int64_t)c->n * g.m_tiles * g.n_tiles;

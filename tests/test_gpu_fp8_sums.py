@@ -45,3 +45,48 @@ def test_sums_behind_a_checkpoint_are_handed_over_every_eight_mmas(B, K, O):
         lost.append(float(((n.ref - y[0].cpu().numpy().astype(np.float64)) / n.ref).mean()))
     assert 0.0 < lost[0] < 2.0 ** -20 and lost[1] <= 0.75 * lost[0], lost
     n.close()
+
+
+# 128 MMAs lose at most a unit each of the accumulator they find: (1 + ... + 128) / 128 * 2^-23 of the sum of magnitudes
+COARSE = 64.5 * 2.0 ** -23
+
+
+def long_rows(rows, K, cancel, seed):
+    """Positive rows; with `cancel` the second half repeats the first (the other factor there has the opposite sign)."""
+    v = np.abs(np.random.default_rng(seed).standard_normal((rows, K))).astype(np.float32)
+    if cancel:
+        v[:, K // 2:] = v[:, :K // 2]
+    return v
+
+
+@pytest.mark.parametrize("K", [16384, 65536])
+@pytest.mark.parametrize("cancel", [False, True])
+def test_bf16_results_of_long_contractions(K, cancel):
+    """bf16 rounds to nearest: half a step, 2^-9 of a value, and on average over R values 2^-8 / sqrt(12 R) either way."""
+    B, O = 64, 512
+    x, w = long_rows(B, K, cancel, K), long_rows(O, K, cancel, K + 1)
+    if cancel:
+        w[:, K // 2:] *= -1.0
+    n = Net(x, w)
+    y = n.ctx.fp8_linear_forward(n.x8, n.w8, dtype=torch.bfloat16)[0].float().cpu().numpy().astype(np.float64)
+    S = np.abs(n.xv) @ np.abs(n.wv).T
+    if cancel:
+        assert not n.ref.any() and (np.abs(y) <= COARSE * S * (1 + 2.0 ** -8)).all(), np.abs(y / S).max()
+    else:
+        assert (np.abs(y - n.ref) <= COARSE * S + 2.0 ** -8 * n.ref).all()
+        assert abs(((n.ref - y) / n.ref).mean()) <= COARSE + 4 * 2.0 ** -8 / (12 * B * O) ** 0.5
+    n.close()
+
+
+def test_bf16_input_gradients_of_many_outputs():
+    """dx adds over the outputs of the layer."""
+    B, K, O = 64, 128, 65536
+    w, dy = long_rows(O, K, False, 1), long_rows(B, O, False, 2)
+    n = Net(long_rows(B, K, False, 3), w)
+    dx = torch.empty((1, B, K), dtype=torch.bfloat16, device="cuda")
+    n.ctx.fp8_linear_backward(n.x8, n.w8, torch.from_numpy(dy[None]).cuda(), w_off=0, dx=dx)
+    ref = fo.load(*fo.save(dy), O) @ n.wv
+    got = dx[0].float().cpu().numpy().astype(np.float64)
+    assert (np.abs(got - ref) <= COARSE * ref + 2.0 ** -8 * ref).all()
+    assert abs(((ref - got) / ref).mean()) <= COARSE + 4 * 2.0 ** -8 / (12 * B * K) ** 0.5
+    n.close()
