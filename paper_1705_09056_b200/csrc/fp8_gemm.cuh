@@ -612,6 +612,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
             }
             if constexpr (MODE == kForward && BN >= 128) {
                 if (g.q) {
+                    // columns beyond the result are 0 in the padding, also in rows that hold a NaN
+                    if (n0 + COLS > g.N) {
+#pragma unroll
+                        for (int j = 0; j < COLS; ++j) sum[j] = n0 + j < g.N ? sum[j] : 0.f;
+                    }
                     // the row's block of 128 columns: this thread's own (BN 256), or shared with the warp of the other half
                     uint32_t top = 0;
 #pragma unroll
