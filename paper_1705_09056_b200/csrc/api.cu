@@ -122,6 +122,9 @@ float band_entry(const dpsgd_ctx* c, int i, int j) {
     return 0.f;
 }
 
+// Whether `size` >= 0 parameters from column `off` on lie inside the parameter row (no sum that could overflow).
+bool block_inside(const dpsgd_ctx* c, int64_t off, int64_t size) { return off >= 0 && off <= c->N && size <= c->N - off; }
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 void release(dpsgd_ctx* c) {
@@ -819,14 +822,14 @@ dpsgd_status check_layer8(dpsgd_ctx* c, const void* xq, const void* xe, int32_t 
         return fail(c, DPSGD_ERR_UNSUPPORTED, "at most 2^20 rows per node and widths of 65536");
     if (!aligned(xq, 16) || !aligned(wq, 16) || !aligned(xe, 4) || !aligned(we, 4))
         return fail(c, DPSGD_ERR_ALIGN, "q buffers must be 16-byte and e buffers 4-byte aligned");
-    if (b_off < -1 || (b_off >= 0 && b_off + d_out > c->N))
+    if (b_off < -1 || (b_off >= 0 && !block_inside(c, b_off, d_out)))
         return fail(c, DPSGD_ERR_ARG, "bias block lies outside the parameter row");
     return DPSGD_OK;
 }
 
 dpsgd_status check_weight_block(dpsgd_ctx* c, int64_t w_off, int32_t d_out, int32_t d_in) {
-    return w_off < 0 || w_off > c->N || (int64_t)d_out * d_in > c->N - w_off
-               ? fail(c, DPSGD_ERR_ARG, "weight block lies outside the parameter row") : DPSGD_OK;
+    return block_inside(c, w_off, (int64_t)d_out * d_in)
+               ? DPSGD_OK : fail(c, DPSGD_ERR_ARG, "weight block lies outside the parameter row");
 }
 }  // namespace
 

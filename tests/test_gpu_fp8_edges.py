@@ -27,3 +27,17 @@ def test_checkpoint_padding_of_rows_with_nan(n, B, K, O):
     assert torch.equal(c.q, ref.q) and torch.equal(c.e, ref.e)
     assert not c.q[..., O:].any()
     l.close()
+
+
+@pytest.mark.parametrize("off", [2 ** 63 - 1, 2 ** 63 - 16, 2 ** 62, -2, -2 ** 63])
+def test_offsets_near_the_ends_of_64_bits_are_refused(off):
+    """offset + size must not wrap round on its way to the comparison with N."""
+    l = Layer(2, 4, 32, 16)
+    y, dy = torch.zeros(2, 4, 16, device="cuda"), torch.zeros(2, 4, 16, device="cuda")
+    for call in (lambda: l.ctx.fp8_linear_forward(l.x8, l.w8, b_off=off, out=y),
+                 lambda: l.ctx.fp8_linear_backward(l.x8, l.w8, dy, w_off=0, b_off=off),
+                 lambda: l.ctx.fp8_linear_backward(l.x8, l.w8, dy, w_off=off),
+                 lambda: l.ctx.fp8_weights(off, 16, 32)):
+        with pytest.raises(binding.DpsgdError):
+            call()
+    l.close()
