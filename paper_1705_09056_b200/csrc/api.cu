@@ -763,8 +763,8 @@ DPSGD_API dpsgd_status dpsgd_conv3x3_forward(dpsgd_ctx* c, const float* in_dev, 
     if (!in_dev || !out_dev) return fail(c, DPSGD_ERR_ARG, "in_dev or out_dev is NULL");
     if (!aligned(in_dev, 16) || !aligned(out_dev, 16)) return fail(c, DPSGD_ERR_ALIGN, "in_dev and out_dev must be 16-byte aligned");
     if (const char* why = conv3x3_forward_unsupported(batch, c_in, h, w, c_out, stride)) return fail(c, DPSGD_ERR_UNSUPPORTED, why);
-    const int64_t wsz = (int64_t)c_out * c_in * 9;
-    if (w_off < 0 || b_off < 0 || w_off + wsz > c->N || b_off + c_out > c->N)
+    const int64_t filters = (int64_t)c_out * c_in;
+    if (filters > c->N / 9 || !block_inside(c, w_off, filters * 9) || !block_inside(c, b_off, c_out))
         return fail(c, DPSGD_ERR_ARG, "filter or bias block lies outside the parameter row");
     const char* why = nullptr;
     cudaError_t e = launch_conv3x3_forward(c, in_dev, batch, c_in, h, w, c_out, stride, w_off, b_off, relu, out_dev, &why);
@@ -783,8 +783,8 @@ DPSGD_API dpsgd_status dpsgd_conv3x3_backward(dpsgd_ctx* c, const float* in_dev,
         return fail(c, DPSGD_ERR_ALIGN, "activation and gradient buffers must be 16-byte aligned");
     if (batch < 1 || c_in < 1 || h < 1 || w < 1 || c_out < 1) return fail(c, DPSGD_ERR_ARG, "sizes must be positive");
     if (stride != 1 && stride != 2) return fail(c, DPSGD_ERR_UNSUPPORTED, "stride must be 1 or 2");
-    const int64_t wsz = (int64_t)c_out * c_in * 9;
-    if (w_off < 0 || b_off < 0 || w_off + wsz > c->N || b_off + c_out > c->N)
+    const int64_t filters = (int64_t)c_out * c_in;
+    if (filters > c->N / 9 || !block_inside(c, w_off, filters * 9) || !block_inside(c, b_off, c_out))
         return fail(c, DPSGD_ERR_ARG, "filter or bias block lies outside the parameter row");
     const char* why = nullptr;
     cudaError_t e = launch_conv3x3_backward(c, in_dev, out_dev, dout_dev, batch, c_in, h, w, c_out, stride, w_off, b_off,
