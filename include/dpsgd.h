@@ -367,13 +367,21 @@ DPSGD_API dpsgd_status dpsgd_fp8_linear_forward(dpsgd_ctx* ctx, const uint8_t* x
  *   dx[i][b][k]              <- sum_o d8[i][b][o] w_i[o][k]    (dx_dev NULL: not wanted)
  * Sums over the minibatch, as in dpsgd_conv3x3_backward: the caller's dy carries the 1/B of a mean loss.
  *   dy_dev  [n][batch][d_out] contiguous, fp32 or bf16;  dx_dev [n][batch][d_in] contiguous, fp32 or bf16
- * The library keeps a workspace of about (3 d_out + 2 d_in) bytes per row (allocated on the first call, grown when a
- * larger layer comes, released by dpsgd_destroy).
+ * The library keeps a workspace of about (3 d_out + 2 d_in) bytes per row (dpsgd_fp8_reserve).
  */
 DPSGD_API dpsgd_status dpsgd_fp8_linear_backward(dpsgd_ctx* ctx, const uint8_t* xq_dev, const uint8_t* xe_dev, int32_t batch,
                                                  int32_t d_in, int32_t d_out, const uint8_t* wq_dev, const uint8_t* we_dev,
                                                  const uint8_t* gate_q_dev, const void* dy_dev, int32_t dy_dtype,
                                                  int64_t w_off, int64_t b_off, void* dx_dev, int32_t dx_dtype);
+
+/*
+ * Workspace of dpsgd_fp8_linear_backward for layers of up to this size, ahead of the first call.  Without it the first
+ * call allocates, and so does a later one with a larger layer; dpsgd_set_model with mlp_precision 3 reserves what the model
+ * needs.  A call that is captured in a CUDA graph must find its workspace reserved (DPSGD_ERR_STATE otherwise, before anything
+ * is recorded); memory that a captured graph uses stays valid until dpsgd_destroy, also when the workspace grows after.
+ * Not to be called during a capture itself unless there is nothing to allocate.
+ */
+DPSGD_API dpsgd_status dpsgd_fp8_reserve(dpsgd_ctx* ctx, int32_t batch, int32_t d_in, int32_t d_out);
 
 /* Output of Algorithm 1: xbar = (1/n) sum_i x_i into xbar_dev (fp32 [ld], 16-byte aligned). */
 DPSGD_API dpsgd_status dpsgd_average(dpsgd_ctx* ctx, float* xbar_dev);

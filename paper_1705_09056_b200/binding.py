@@ -58,6 +58,7 @@ SIGNATURES = {
     "dpsgd_fp8_weights": [_vp, _i64, _i32, _i32, _vp, _vp],
     "dpsgd_fp8_linear_forward": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i32, _vp, _vp],
     "dpsgd_fp8_linear_backward": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _vp, _i32],
+    "dpsgd_fp8_reserve": [_vp, _i32, _i32, _i32],
     "dpsgd_mix_update_host": [_vp, _vp, _i64, ctypes.POINTER(ctypes.c_double)],
     "dpsgd_consensus_dist_noalloc": [_vp, _i32, _i64, _i64, _vp, _vp],
     "dpsgd_current": [_vp, ctypes.POINTER(_vp)],
@@ -419,6 +420,11 @@ class Dpsgd:
                                                         w.q.data_ptr(), w.e.data_ptr(), gp, dy.data_ptr(), DTYPES[dy.dtype],
                                                         w_off, b_off, xp, xt))
         return dx
+
+    def fp8_reserve(self, batch: int, d_in: int, d_out: int) -> None:
+        """Workspace of fp8_linear_backward for layers of up to this size: before the first call that must not allocate, and
+        before a call is captured in a CUDA graph."""
+        self._check(self._lib.dpsgd_fp8_reserve(self._h, batch, d_in, d_out))
 
     def average(self, xbar: Optional[torch.Tensor] = None) -> torch.Tensor:
         if xbar is None:

@@ -146,6 +146,7 @@ void release(dpsgd_ctx* c) {
     cudaFree(c->d_partials);
     cudaFree(c->d_conv_ws);
     cudaFree(c->d_fp8_ws);
+    for (uint8_t* p : c->fp8_ws_kept) cudaFree(p);
     cudaFree(c->d_mlp8);
     cudaFree(c->d_result);
     if (c->h_result) cudaFreeHost(c->h_result);
@@ -368,6 +369,7 @@ DPSGD_API dpsgd_status dpsgd_set_model(dpsgd_ctx* c, int32_t kind, const int32_t
     if (e == cudaSuccess) e = cudaMalloc(&c->d_coef, sizeof(float) * (size_t)c->n * batch);
     if (e == cudaSuccess && kind == DPSGD_MODEL_MLP && mlp_precision == 3) {
         e = cudaMalloc(&c->d_mlp8, mlp8_bytes(c));
+        for (int l = 0; l < shape.nlayers && e == cudaSuccess; ++l) e = reserve_fp8_workspace(c, batch, shape.dims[l], shape.dims[l + 1]);
     } else if (e == cudaSuccess && kind == DPSGD_MODEL_MLP) {
         c->act_floats = mlp_act_floats(c);
         c->delta_floats = mlp_delta_floats(c);
@@ -795,6 +797,7 @@ DPSGD_API dpsgd_status dpsgd_conv3x3_backward(dpsgd_ctx* c, const float* in_dev,
 
 namespace {
 constexpr int kMaxBatch8 = 1 << 20;
+constexpr const char* kReserveFirst = "reserve the workspace (dpsgd_fp8_reserve) before the call is captured in a graph";
 
 dpsgd_status check_dtype(dpsgd_ctx* c, int32_t dtype) {
     return dtype == DPSGD_F32 || dtype == DPSGD_BF16 ? DPSGD_OK : fail(c, DPSGD_ERR_ARG, "dtype must be DPSGD_F32 or DPSGD_BF16");
@@ -814,12 +817,18 @@ dpsgd_status check_rows8(dpsgd_ctx* c, const void* x, int32_t dtype, int64_t ld,
     return DPSGD_OK;
 }
 
-dpsgd_status check_layer8(dpsgd_ctx* c, const void* xq, const void* xe, int32_t batch, int32_t d_in, int32_t d_out,
-                          const void* wq, const void* we, int64_t b_off) {
-    if (!xq || !xe || !wq || !we) return fail(c, DPSGD_ERR_ARG, "checkpoint or weight buffer is NULL");
+dpsgd_status check_sizes8(dpsgd_ctx* c, int32_t batch, int32_t d_in, int32_t d_out) {
     if (batch < 1 || d_in < 1 || d_out < 1) return fail(c, DPSGD_ERR_ARG, "sizes must be positive");
     if (batch > kMaxBatch8 || d_in > kMaxWidth8 || d_out > kMaxWidth8)
         return fail(c, DPSGD_ERR_UNSUPPORTED, "at most 2^20 rows per node and widths of 65536");
+    return DPSGD_OK;
+}
+
+dpsgd_status check_layer8(dpsgd_ctx* c, const void* xq, const void* xe, int32_t batch, int32_t d_in, int32_t d_out,
+                          const void* wq, const void* we, int64_t b_off) {
+    if (!xq || !xe || !wq || !we) return fail(c, DPSGD_ERR_ARG, "checkpoint or weight buffer is NULL");
+    const dpsgd_status s = check_sizes8(c, batch, d_in, d_out);
+    if (s != DPSGD_OK) return s;
     if (!aligned(xq, 16) || !aligned(wq, 16) || !aligned(xe, 4) || !aligned(we, 4))
         return fail(c, DPSGD_ERR_ALIGN, "q buffers must be 16-byte and e buffers 4-byte aligned");
     if (b_off < -1 || (b_off >= 0 && !block_inside(c, b_off, d_out)))
@@ -894,7 +903,17 @@ DPSGD_API dpsgd_status dpsgd_fp8_linear_backward(dpsgd_ctx* c, const uint8_t* xq
     if ((s = check_weight_block(c, w_off, d_out, d_in)) != DPSGD_OK) return s;
     const cudaError_t err = launch_fp8_backward(c, xq, xe, wq, we, gate_q, dy, dy_dtype, batch, d_in, d_out, c->G + w_off,
                                                 b_off >= 0 ? c->G + b_off : nullptr, dx, dx_dtype);
+    if (err == cudaErrorStreamCaptureUnsupported) return fail(c, DPSGD_ERR_STATE, kReserveFirst);
     return err == cudaSuccess ? DPSGD_OK : cuda_fail(c, err, "8-bit layer backward kernels");
+}
+
+DPSGD_API dpsgd_status dpsgd_fp8_reserve(dpsgd_ctx* c, int32_t batch, int32_t d_in, int32_t d_out) {
+    if (!c) return DPSGD_ERR_ARG;
+    const dpsgd_status s = check_sizes8(c, batch, d_in, d_out);
+    if (s != DPSGD_OK) return s;
+    const cudaError_t err = reserve_fp8_workspace(c, batch, d_in, d_out);
+    if (err == cudaErrorStreamCaptureUnsupported) return fail(c, DPSGD_ERR_STATE, kReserveFirst);
+    return err == cudaSuccess ? DPSGD_OK : cuda_fail(c, err, "workspace of the 8-bit layers");
 }
 
 DPSGD_API dpsgd_status dpsgd_average(dpsgd_ctx* c, float* xbar) {

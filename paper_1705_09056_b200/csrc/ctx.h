@@ -131,6 +131,8 @@ struct dpsgd_ctx {
     // backward of the 8-bit layers: output gradient in 8 bits and in bf16, input checkpoint in bf16, bias partial sums
     uint8_t* d_fp8_ws = nullptr;
     size_t fp8_ws_bytes = 0;
+    bool fp8_ws_captured = false;         // a graph of the caller's was recorded on d_fp8_ws
+    std::vector<uint8_t*> fp8_ws_kept;    // outgrown, but recorded in such a graph
 
     uint8_t* d_mlp8 = nullptr;   // MLP with 8-bit layers: checkpoints, weights, logits and errors (grad_mlp8.cu)
 
@@ -210,6 +212,7 @@ cudaError_t launch_delta(dpsgd_ctx* c, const void* dy, int dtype, int B, int O, 
 // 8-bit layers (fp8_linear.cu)
 cudaError_t launch_fp8_forward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* xe, const uint8_t* wq, const uint8_t* we,
                                int B, int K, int O, const float* bias, int relu, void* y, int dtype, uint8_t* yq, uint8_t* ye);
+cudaError_t reserve_fp8_workspace(dpsgd_ctx* c, int B, int K, int O);
 cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* xe, const uint8_t* wq, const uint8_t* we,
                                 const uint8_t* gate, const void* dy, int dy_dtype, int B, int K, int O, float* gw,
                                 float* gb, void* dx, int dx_dtype);

@@ -1,6 +1,7 @@
 // Host side of the 8-bit layers: tile shapes, tensor maps and the launches of one forward or backward pass over all
 // nodes.  The kernels are in fp8_gemm.cuh (products) and ckpt8.cu (everything that only moves data).
 #include <algorithm>
+#include <new>
 
 #include "ctx.h"
 #include "fp8_gemm.cuh"
@@ -95,9 +96,52 @@ void set_out(Args& g, void* out, int dtype, int rows, int cols) {
     g.out_vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && g.out_pitch % 16 == 0;
 }
 
-size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+// Workspace of a backward pass: d in 8 bits | its exponents | d in bf16 | x in bf16 | bias partial sums
+struct Workspace {
+    int64_t ldv, ldx;                      // elements between rows of the bf16 copies
+    size_t e, v, x, parts, total;          // byte offsets
+};
+Workspace make_workspace(const dpsgd_ctx* c, int B, int K, int O) {
+    const auto round_up = [](size_t v) { return (v + 255) / 256 * 256; };
+    const size_t rows = (size_t)c->n * B;
+    const int chunks = delta_chunks(B);
+    Workspace w{};
+    w.ldv = (O + 7) / 8 * 8; w.ldx = (K + 7) / 8 * 8;
+    w.e = round_up(rows * f8::q_pitch(O));
+    w.v = w.e + round_up(rows * f8::e_pitch(O));
+    w.x = w.v + round_up(rows * w.ldv * 2);
+    w.parts = w.x + round_up(rows * w.ldx * 2);
+    w.total = w.parts + (chunks > 1 ? round_up((size_t)c->n * chunks * O * 4) : 0);
+    return w;
+}
 
 }  // namespace
+
+// The workspace holds nothing between calls, but a graph that a caller captures holds its address: what such a graph was
+// recorded on is kept until the context goes, and a capture that would need a larger one is refused before it records.
+cudaError_t reserve_fp8_workspace(dpsgd_ctx* c, int B, int K, int O) {
+    const size_t need = make_workspace(c, B, K, O).total;
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    bool capturing = true;                                          // also where the legacy stream cannot be asked during one
+    if (cudaStreamIsCapturing(c->stream, &status) == cudaSuccess) capturing = status != cudaStreamCaptureStatusNone;
+    else cudaGetLastError();
+    if (need > c->fp8_ws_bytes) {
+        if (capturing) return cudaErrorStreamCaptureUnsupported;
+        if (c->fp8_ws_captured) {
+            try { c->fp8_ws_kept.push_back(c->d_fp8_ws); } catch (const std::bad_alloc&) { return cudaErrorMemoryAllocation; }
+        } else {
+            cudaFree(c->d_fp8_ws);
+        }
+        c->d_fp8_ws = nullptr;
+        c->fp8_ws_bytes = 0;
+        c->fp8_ws_captured = false;
+        const cudaError_t e = cudaMalloc(&c->d_fp8_ws, need);
+        if (e != cudaSuccess) { c->d_fp8_ws = nullptr; return e; }
+        c->fp8_ws_bytes = need;
+    }
+    c->fp8_ws_captured |= capturing;
+    return cudaSuccess;
+}
 
 cudaError_t launch_fp8_forward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* xe, const uint8_t* wq, const uint8_t* we,
                                int B, int K, int O, const float* bias, int relu, void* y, int dtype, uint8_t* yq,
@@ -124,29 +168,17 @@ cudaError_t launch_fp8_forward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* x
 cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* xe, const uint8_t* wq, const uint8_t* we,
                                 const uint8_t* gate, const void* dy, int dy_dtype, int B, int K, int O, float* gw,
                                 float* gb, void* dx, int dx_dtype) {
-    // workspace: d in 8 bits | its exponents | d in bf16 | x in bf16 | bias partial sums
-    const int64_t rows = (int64_t)c->n * B;
-    const int64_t ldv = (O + 7) / 8 * 8, ldx = (K + 7) / 8 * 8;
-    const size_t n_q = round_up((size_t)rows * f8::q_pitch(O)), n_e = round_up((size_t)rows * f8::e_pitch(O));
-    const size_t n_v = round_up((size_t)rows * ldv * 2), n_x = round_up((size_t)rows * ldx * 2);
-    const int chunks = delta_chunks(B);
-    const size_t n_p = chunks > 1 && gb ? round_up((size_t)c->n * chunks * O * 4) : 0;
-    const size_t need = n_q + n_e + n_v + n_x + n_p;
-    if (need > c->fp8_ws_bytes) {
-        cudaFree(c->d_fp8_ws);
-        c->d_fp8_ws = nullptr;
-        c->fp8_ws_bytes = 0;
-        cudaError_t e = cudaMalloc(&c->d_fp8_ws, need);
-        if (e != cudaSuccess) return e;
-        c->fp8_ws_bytes = need;
-    }
+    cudaError_t e = reserve_fp8_workspace(c, B, K, O);
+    if (e != cudaSuccess) return e;
+    const Workspace ws = make_workspace(c, B, K, O);
+    const int64_t ldv = ws.ldv, ldx = ws.ldx;
     uint8_t* dq = c->d_fp8_ws;
-    uint8_t* de = dq + n_q;
-    uint8_t* dv = de + n_e;
-    uint8_t* xv = dv + n_v;
-    float* parts = reinterpret_cast<float*>(xv + n_x);
+    uint8_t* de = dq + ws.e;
+    uint8_t* dv = dq + ws.v;
+    uint8_t* xv = dq + ws.x;
+    float* parts = reinterpret_cast<float*>(dq + ws.parts);
 
-    cudaError_t e = launch_delta(c, dy, dy_dtype, B, O, gate, dx ? dq : nullptr, de, dv, ldv, parts, gb, xq, xe, K, xv, ldx);
+    e = launch_delta(c, dy, dy_dtype, B, O, gate, dx ? dq : nullptr, de, dv, ldv, parts, gb, xq, xe, K, xv, ldx);
     if (e != cudaSuccess) return e;
     Args g{};
     g.M = K; g.N = O; g.K = B;

@@ -41,3 +41,81 @@ def test_offsets_near_the_ends_of_64_bits_are_refused(off):
         with pytest.raises(binding.DpsgdError):
             call()
     l.close()
+
+
+def free_bytes():
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info()[0]
+
+
+def test_set_model_allocates_all_that_a_gradient_needs():
+    """A hidden layer wider than the later ones: no allocation, hence no device synchronisation, inside the gradient."""
+    w = wl.mlp_workload(n=4, dims=(64, 1024, 2048, 10), m=64, batch=512, gamma=0.05, seed=1)
+    A, y = w.A.cuda(), w.y.cuda()
+    for again in (False, True):                      # the first context also loads the kernels
+        run = GpuRun(4, w.N, w.csr(), w.gamma, seed=1, X=np.tile(w.x0.numpy(), (4, 1)))
+        run.ctx.set_model(w.model, w.dims, 0.0, 512, 3)
+        run.ctx.set_data(A, y)
+        before = free_bytes()
+        run.ctx.grad(0)
+        assert not again or free_bytes() == before
+        run.ctx.sync()
+        run.close()
+
+
+def test_reserve_allocates_what_a_backward_needs():
+    for again in (False, True):
+        l = Layer(3, 300, 1000, 1004)
+        dy, dx = torch.randn(3, 300, 1004, device="cuda"), torch.empty(3, 300, 1000, device="cuda")
+        l.ctx.fp8_reserve(301, 1000, 1010)           # layers of up to this size
+        before = free_bytes()
+        l.ctx.fp8_linear_backward(l.x8, l.w8, dy, w_off=0, b_off=l.b_off, dx=dx)
+        assert not again or free_bytes() == before
+        l.close()
+
+
+def test_reserve_refusals():
+    l = Layer(1, 2, 32, 16)
+    r, h = l.ctx._lib.dpsgd_fp8_reserve, l.ctx._h
+    assert r(None, 1, 1, 1) == r(h, 0, 1, 1) == r(h, 1, -1, 1) == r(h, 1, 1, 0) == binding.ERR_ARG
+    assert r(h, 1, 65537, 1) == r(h, (1 << 20) + 1, 1, 1) == binding.ERR_UNSUPPORTED
+    assert r(h, 1, 1, 1) == binding.OK
+    l.close()
+
+
+def test_captured_backward_keeps_its_workspace():
+    """Without a reserved workspace a capture is refused before it records anything; a graph that was captured computes
+    the same after a larger layer has made the workspace grow and others have taken the memory that is free."""
+    n, B, K, O = 2, 150, 520, 600
+    l = Layer(n, B, K, O)
+    s = torch.cuda.Stream()
+    l.ctx.bind(l.g.X0, l.g.X1, l.g.G, stream=s)
+    dy, dx = torch.randn(n, B, O, device="cuda"), torch.empty(n, B, K, device="cuda")
+    call = lambda: l.ctx.fp8_linear_backward(l.x8, l.w8, dy, w_off=0, b_off=l.b_off, dx=dx)   # noqa: E731
+    torch.cuda.synchronize()
+    empty = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(empty, stream=s):
+        with pytest.raises(binding.DpsgdError) as e:
+            call()
+        dy.add_(0.0)                                 # the capture is still intact
+    assert "reserve" in str(e.value)
+    l.ctx.fp8_reserve(B, K, O)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call()
+    graph.replay()
+    torch.cuda.synchronize()
+    G, D = l.g.G.clone(), dx.clone()
+    for i in range(n):
+        ref, _ = fo.backward(l.xv[i], l.wv[i], dy[i].cpu().numpy(), None)
+        assert np.abs(D[i].cpu().numpy() - ref[2]).max() <= 1e-4 * np.abs(ref[2]).max()
+    l.ctx.fp8_reserve(16 * B, K, O)                  # grows
+    junk = torch.full((256 << 20,), 0x7F, dtype=torch.uint8, device="cuda")
+    l.g.G.fill_(3.0), dx.fill_(3.0)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(l.g.G[:, :l.N], G[:, :l.N]) and torch.equal(dx, D)
+    assert bool((junk == 0x7F).all())
+    del graph, empty
+    l.close()
