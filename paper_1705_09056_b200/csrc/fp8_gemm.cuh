@@ -84,7 +84,6 @@ struct Args {
     uint8_t* qe; int64_t qe_pitch;
     const float* bias; int64_t bias_node;            // kForward; NULL: none
     int relu;
-    int wait_last;                                   // the inputs are complete at launch: wait for the predecessor at the end
     int hand;                                        // k-blocks after which an accumulator is handed over
     uint32_t a_rows;                                 // rows of A a stage loads (8 .. 128);  kWeight: samples it loads (16 .. 64)
     uint32_t a_bytes, block_bytes;                   // of a k-block: A, and A with B; a stage is Shape::KPS of them
@@ -342,10 +341,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     else __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    // kWeight lets its successor start after its own wait: that one (wait_last) relies on everything before this kernel
-    if (MODE != kWeight) chain_next();
-    if (!g.wait_last) chain_wait();
-    if (MODE == kWeight) chain_next();
+    chain_next();
+    chain_wait();
     const int per_node = g.m_tiles * g.n_tiles;
     bool ok = true;
 
@@ -651,7 +648,6 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
         }
         if (!ok && lane == 0) atomicExch(g.status, (int)DPSGD_ERR_TIMEOUT);
     }
-    if (g.wait_last) chain_wait();      // its completion stands for its predecessor's, as that of every kernel of a chain
     tc::tc_fence_before();
     if (PAIR) cluster_sync();       // neither CTA leaves while the other may still reach its shared memory
     else __syncthreads();

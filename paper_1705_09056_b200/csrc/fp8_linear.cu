@@ -72,8 +72,7 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool f
 // epilogue with the next tile, are level with wider ones or better.  With more rows it is bound by what the operands bring
 // from L2 (about 64 bytes per cycle and SM): pairs of CTAs share a tile of 256 rows and 256 columns, 32 KB per CTA and
 // k-block instead of 48 for 128 rows and 256 columns, unless such tiles leave far more SMs idle in the last round (training
-// forward of 4 nodes 4096x4096x4096: 300 against 314 us).  kInput keeps to single CTAs of 256 columns: it starts beside the
-// last tiles of the weight gradient, where SMs become free one by one, and a pair needs two of them (the backward of those
+// forward of 4 nodes 4096x4096x4096: 300 against 314 us).  kInput keeps to single CTAs of 256 columns (the backward of those
 // nodes: level within the noise, 816-844 us either way).
 template <int MODE>
 cudaError_t launch_wide(dpsgd_ctx* c, const Operands& o, const Args& g, bool precise, bool fine = false) {
@@ -186,20 +185,18 @@ cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* 
     g.out_node = c->ld * 4;
     const Operands w{xv, dv, ldx * 2, ldv * 2};
     // A gradient that streams to HBM, from few samples: pairs of CTAs, which read the operands a third less (112 nodes
-    // 64x2048x2048, 1.9 GB: 497 against 535 us for the backward).  One that stays in L2 or has many samples: single CTAs,
-    // which dx can fill up one by one (32 nodes 32x784x1024: 32.8 against 41.8 us; 7 nodes 77x1001x1003: 23.9 against 28.0).
+    // 64x2048x2048, 1.9 GB: 497 against 535 us for the backward).  One that stays in L2 or has many samples: single CTAs
+    // (32 nodes 32x784x1024: 32.8 against 41.8 us; 7 nodes 77x1001x1003: 23.9 against 28.0).
     const bool stream = K > kTileM && B <= kSegment * 64 && (double)c->n * K * O * 4.0 >= 512.0 * 1024 * 1024;
     e = stream ? launch<kWeight, 256, true>(c, w, g, true) : launch<kWeight, 256, false>(c, w, g, true);
     if (e != cudaSuccess || !dx) return e;
-    // The weight gradient lets its successor start only after it has itself waited for the launch above, so all that dx is
-    // formed from is there when this kernel begins: it runs beside the weight gradient's last tiles and waits for that
-    // kernel at its own end (the backward of 32 nodes 32x784x1024 takes 33.5 us so, 36.9 us one after the other; 7 nodes
-    // 77x1001x1003 24.4 and 25.7 us).
+    // dx waits for the weight gradient, although it needs the launch before it only: a kernel may read what it has not itself
+    // waited for only at its own risk (33.0 us without the wait against 36.0 on 32 nodes 32x784x1024, 23.9 against 25.3 on 7
+    // nodes 77x1001x1003).
     Args h{};
     h.M = B; h.N = K; h.K = O;
     h.ae = de; h.ae_pitch = f8::e_pitch(O);
     h.we = we; h.we_pitch = f8::e_pitch(K); h.we_node = h.we_pitch * ((O + f8::kBlock - 1) / f8::kBlock);
-    h.wait_last = 1;
     set_out(h, dx, dx_dtype, B, K);
     return launch_wide<kInput>(c, Operands{dq, wq, f8::q_pitch(O), f8::q_pitch(K)}, h, dx_dtype == DPSGD_F32);
 }

@@ -8,8 +8,8 @@
 namespace dpsgd {
 
 // chain_next() at a kernel's start lets its successor begin (all CTAs are resident once the last has called it, so the
-// successor takes no room from it); a kernel launched with launch_chained calls chain_wait() before it touches memory, or,
-// where its inputs are known to be complete when it starts, before it ends.
+// successor takes no room from it); a kernel launched with launch_chained calls chain_wait() before it touches memory.  Only
+// a kernel that waits is promised to see what the kernels before it have written, whatever they have waited for themselves.
 __device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
