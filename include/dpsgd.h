@@ -114,7 +114,8 @@ DPSGD_API dpsgd_status dpsgd_bind(dpsgd_ctx* ctx, float* X0_dev, float* X1_dev, 
  * product (faster, about 1e-3 relative on G), 2 = fp32 FMA kernel always, 3 = 8-bit layers: the activations are kept as
  * 8-bit checkpoints, all three products of a layer take 8-bit operands (see the 8-bit forms below; the error passed
  * between layers is bf16 before it is rounded), logits, softmax, parameters and G stay fp32.  With 3 the gossip step is
- * a stage of its own (dpsgd_set_fused_step does not apply) and layer widths are at most 65536.
+ * a stage of its own (dpsgd_set_fused_step does not apply) and layer widths are at most 65536.  Any other value of an MLP is
+ * DPSGD_ERR_ARG.
  */
 DPSGD_API dpsgd_status dpsgd_set_model(dpsgd_ctx* ctx, int32_t kind, const int32_t* dims_host,
                              int32_t ndims, float l2_lambda, int32_t batch,

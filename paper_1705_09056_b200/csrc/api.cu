@@ -337,6 +337,7 @@ DPSGD_API dpsgd_status dpsgd_set_model(dpsgd_ctx* c, int32_t kind, const int32_t
     } else if (kind == DPSGD_MODEL_MLP) {
         if (ndims < 2 || ndims - 1 > kMaxLayers)
             return fail(c, DPSGD_ERR_UNSUPPORTED, "MLP needs 1..8 weight layers");
+        if (mlp_precision < 0 || mlp_precision > 3) return fail(c, DPSGD_ERR_ARG, "mlp_precision must be 0, 1, 2 or 3");
         shape.nlayers = ndims - 1;
         for (int t = 0; t < ndims; ++t) shape.dims[t] = dims[t];
         for (int l = 0; l < shape.nlayers; ++l) {

@@ -119,3 +119,19 @@ def test_captured_backward_keeps_its_workspace():
     assert bool((junk == 0x7F).all())
     del graph, empty
     l.close()
+
+
+@pytest.mark.parametrize("precision", [-1, 4, 8, 2 ** 31 - 1])
+def test_precisions_that_do_not_exist_are_refused(precision):
+    """3 stands for 8-bit layers; a number beside the four must not run as some other precision.  Linear models have none."""
+    w = wl.mlp_workload(n=2, dims=(16, 20, 4), m=16, batch=4, gamma=0.05, seed=1)
+    run = GpuRun(2, w.N, w.csr(), w.gamma)
+    with pytest.raises(binding.DpsgdError) as e:
+        run.ctx.set_model(w.model, w.dims, 0.0, 4, precision)
+    assert e.value.status == binding.ERR_ARG
+    for ok in (0, 1, 2, 3):
+        run.ctx.set_model(w.model, w.dims, 0.0, 4, ok)
+    run.close()
+    lin = GpuRun(2, 16, wl.topology("ring", 2), 0.1)
+    lin.ctx.set_model(binding.MODEL_LSQ, [16], 0.0, 4, precision)
+    lin.close()
