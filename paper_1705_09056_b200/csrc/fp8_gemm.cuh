@@ -115,8 +115,12 @@ template <int MODE, int BN, bool PAIR> struct Shape {
     static constexpr int FIRST_EPI = SCALED ? 8 : 4;               // warps 4-7 write scales where there are any
     static constexpr int THREADS = 32 * (FIRST_EPI + kEpiWarps);
     // registers per thread: launched with 65536 / THREADS rounded down to a multiple of 8 (128 or 168); the first
-    // FIRST_EPI warps give theirs to the epilogue: 256 * 72 + 256 * 184 = 512 * 128, 128 * 80 + 256 * 208 < 384 * 168
-    static constexpr int REGS_FEW = SCALED ? 72 : 80, REGS_EPI = SCALED ? 184 : 208;
+    // FIRST_EPI warps give theirs to the epilogue: 256 * 88 + 256 * 168 = 256 * 72 + 256 * 184 = 512 * 128,
+    // 128 * 80 + 256 * 208 < 384 * 168.  With 72 / 184 the scale warps spill, but for kInput of 128 columns (the pair of 256
+    // columns 138 bytes of stores and 628 of loads: 302 us for the forward of 4 nodes 4096x4096x4096; with 88 / 168 16 and 184:
+    // 297 us); with 96 / 160 the epilogue of 256 columns does.  kInput of 128 columns is level or better with 72 / 184 (backward
+    // of 32 nodes 32x784x1024: 36.1 against 36.6 us).
+    static constexpr int REGS_FEW = !SCALED ? 80 : MODE == kInput && BN == 128 ? 72 : 88, REGS_EPI = SCALED ? 256 - REGS_FEW : 208;
 };
 
 // Shared-memory descriptor of an operand stored with the 128-byte swizzle.  k contiguous: rows of 128 bytes, 8-row
