@@ -68,6 +68,7 @@ constexpr uint32_t kStageOut = 4096;                 // shared memory per epilog
 constexpr uint32_t kSmemLimit = 232448;              // 227 KB per CTA
 constexpr int kSegment = 4;                          // k-blocks per scale word, and per accumulator handed over
 constexpr int kFineHand = 2, kCoarseHand = 32;       // the same where the result is rounded to 8 bits, to bf16
+constexpr int kPairSamples = 128;                    // samples of a weight gradient that pairs of CTAs take at most
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kScaleCol = 256, kScaleSet = 16;  // scale columns of a segment: 4 for A, up to 8 for B
 constexpr int kScaleSets = 4;
@@ -532,9 +533,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
             const int n0 = nt * BN + half * COLS;
             const int rows = g.M - m0;                              // valid rows of this warp (may be <= 0)
             if constexpr (MODE == kWeight) {
-                // Few samples: the tile is one accumulator and the time is that of its stores.  32 columns at a time, so
-                // that the stores of one piece drain while the next is read from tensor memory.
-                if (SEGS == 1) {
+                // Few samples (all that a pair of CTAs is given): the tile is one accumulator and the time is that of its
+                // stores.  32 columns at a time, so that the stores of one piece drain while the next is read from tensor
+                // memory.
+                static_assert(kPairSamples <= kSegment * S::KB, "one accumulator");
+                if (PAIR || SEGS == 1) {
                     const uint32_t ab = acc_i % ACCS;
                     const bool go = mbar_wait(acc_full + ab, (acc_i / ACCS) & 1u);
                     if (!__all_sync(0xffffffffu, go)) { ok = false; break; }

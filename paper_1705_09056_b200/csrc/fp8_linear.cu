@@ -184,10 +184,12 @@ cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* 
     g.out = reinterpret_cast<uint8_t*>(gw);
     g.out_node = c->ld * 4;
     const Operands w{xv, dv, ldx * 2, ldv * 2};
-    // A gradient that streams to HBM, from few samples: pairs of CTAs, which read the operands a third less (112 nodes
-    // 64x2048x2048, 1.9 GB: 497 against 535 us for the backward).  One that stays in L2 or has many samples: single CTAs
-    // (32 nodes 32x784x1024: 32.8 against 41.8 us; 7 nodes 77x1001x1003: 23.9 against 28.0).
-    const bool stream = K > kTileM && B <= kSegment * 64 && (double)c->n * K * O * 4.0 >= 512.0 * 1024 * 1024;
+    // A gradient well beyond L2 from at most two k-blocks of samples: pairs of CTAs, which read the operands a third less.
+    // Otherwise single CTAs, whose stores start sooner.  Without dx, single CTAs against pairs, us: 64 samples of 1024x1024 on
+    // 64 nodes (256 MiB) 56.3 / 61.0, 96 88.0 / 87.9, 128 (512 MiB) 121.8 / 116.5, 256 260 / 235; of 2048x2048 on 32 nodes
+    // (512 MiB) 107 / 109, 40 137 / 133, 112 434 / 372; 128 samples on these 471 / 429, 192 486 / 501, 256 448 / 525; 1024
+    // samples on 64 nodes 674 / 691; 4096 samples of 4096x4096 on 4 nodes 478 / 500.
+    const bool stream = K > kTileM && B <= kPairSamples && (double)c->n * K * O * 4.0 >= 512.0 * 1024 * 1024;
     e = stream ? launch<kWeight, 256, true>(c, w, g, true) : launch<kWeight, 256, false>(c, w, g, true);
     if (e != cudaSuccess || !dx) return e;
     // dx waits for the weight gradient, although it needs the launch before it only: a kernel may read what it has not itself

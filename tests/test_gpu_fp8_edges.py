@@ -6,7 +6,7 @@ import torch
 from oracle import fp8_oracle as fo
 from paper_1705_09056_b200 import binding, workloads as wl
 from tests.gpu_util import GpuRun
-from tests.test_gpu_fp8_layers import Layer
+from tests.test_gpu_fp8_layers import TOL_SUM, Layer
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +135,25 @@ def test_precisions_that_do_not_exist_are_refused(precision):
     lin = GpuRun(2, 16, wl.topology("ring", 2), 0.1)
     lin.ctx.set_model(binding.MODEL_LSQ, [16], 0.0, 4, precision)
     lin.close()
+
+
+@pytest.mark.parametrize("B", [65, 128, 129])
+def test_weight_gradient_beyond_l2_on_both_sides_of_the_sample_limit(B):
+    """546 MB of gradient, two k-blocks of samples on pairs of CTAs and three on single ones; first and last node."""
+    n, K, O = 70, 1500, 1300
+    N = O * K
+    ld = wl.padded_ld(N)
+    X = torch.zeros(n, ld, device="cuda")
+    X[:, :N].normal_()
+    G = torch.full_like(X, 3.0)
+    ctx = binding.Dpsgd(n, N, *wl.ring(n), gamma=0.1)
+    ctx.bind(X, torch.zeros_like(X), G)
+    x, dy = torch.randn(n, B, K, device="cuda"), torch.randn(n, B, O, device="cuda")
+    ctx.fp8_linear_backward(ctx.ckpt8_save(x), ctx.fp8_weights(0, O, K), dy, w_off=0)
+    ctx.sync()
+    assert bool((G[:, N:] == 3.0).all())
+    for i in (0, n - 1):
+        xv, d8 = fo.load(*fo.save(x[i].cpu().numpy()), K), fo.load(*fo.save(dy[i].cpu().numpy()), O)
+        got = G[i, :N].view(O, K).cpu().numpy().astype(np.float64)
+        assert (np.abs(got - d8.T @ xv) <= TOL_SUM * (np.abs(d8).T @ np.abs(xv))).all()
+    ctx.close()
