@@ -361,8 +361,9 @@ DPSGD_API dpsgd_status dpsgd_fp8_linear_forward(dpsgd_ctx* ctx, const uint8_t* x
 
 /*
  * Backward of the same layer from its 8-bit checkpoints (gradient half of Algorithm 1 step 3).  With
- * d = dy * [y > 0] where gate_q_dev holds the q bytes of y's checkpoint (a ReLU layer; ReLU'(0) = 0), d = dy where it is
- * NULL, and d8 the values of d in 8 bits (a scale per 128 elements of a row):
+ * d = dy where y > 0 and 0 elsewhere, whatever dy is there (NaN and infinities too), where gate_q_dev holds the q bytes of
+ * y's checkpoint (a ReLU layer; ReLU'(0) = 0; zeros of either sign, negative bytes and NaN are not > 0), d = dy where it is
+ * NULL, and d8 the values of d in 8 bits (a scale per 128 elements of a row; not finite: NaN):
  *   G[i][w_off + o d_in + k] <- sum_b d8[i][b][o] x[i][b][k]
  *   G[i][b_off + o]          <- sum_b d[i][b][o]               (b_off = -1: not wanted)
  *   dx[i][b][k]              <- sum_o d8[i][b][o] w_i[o][k]    (dx_dev NULL: not wanted)

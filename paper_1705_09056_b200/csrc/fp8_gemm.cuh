@@ -10,7 +10,8 @@
 // exponents of 512 consecutive k form one 32-bit word of a row's scale operand and k-block t uses byte t % 4: a scale
 // costs nothing in the inner loop and no partial sum leaves the tensor core for it.  In kWeight the scales of both
 // operands change from one step of the contraction (a sample) to the next, which the block-scaled form cannot express;
-// E4M3 times a power of two is exact in bf16, so that product runs on kind::f16 at half the 8-bit rate, without rounding.
+// E4M3 times 2^(e - 127) is exact in bf16 for e >= 3 (blocks whose largest magnitude is above 2^-116; below, what falls under
+// 2^-133 is lost), so that product runs on kind::f16 at half the 8-bit rate, without rounding.
 //
 // A tile belongs to one CTA (128 rows) or to a pair of CTAs in a cluster (PAIR: 256 rows x 256 columns, tcgen05 with
 // cta_group::2): each CTA of a pair keeps 128 rows of A and half the columns of B in shared memory and 128 rows of the
