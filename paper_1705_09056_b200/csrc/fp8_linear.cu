@@ -72,8 +72,8 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool f
 // epilogue with the next tile, are level with wider ones or better.  With more rows it is bound by what the operands bring
 // from L2 (about 64 bytes per cycle and SM): pairs of CTAs share a tile of 256 rows and 256 columns, 32 KB per CTA and
 // k-block instead of 48 for 128 rows and 256 columns, unless such tiles leave far more SMs idle in the last round (training
-// forward of 4 nodes 4096x4096x4096: 293 us, 312 from single CTAs of 256 columns, 393 of 128).  kInput keeps to single CTAs of 256 columns (the backward of those
-// nodes: level within the noise, 816-844 us either way).
+// forward of 4 nodes 4096x4096x4096: 293 us, 312 from single CTAs of 256 columns, 393 of 128).  kInput keeps to single CTAs of
+// 256 columns (the backward of those nodes: level within the noise, 816-844 us either way).
 template <int MODE>
 cudaError_t launch_wide(dpsgd_ctx* c, const Operands& o, const Args& g, bool precise, bool fine = false) {
     const int64_t sms = sm_count(c);
