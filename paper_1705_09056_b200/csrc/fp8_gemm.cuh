@@ -28,14 +28,14 @@
 //   epilogue      (8) tcgen05.ld, bias, ReLU, rounding; a warp turns its 32 rows round in 4 KB of shared memory and writes
 //                 whole 128-byte lines
 // The tensor core truncates when it adds to an fp32 accumulator.  Where that can be seen in the result (fp32, or 8 bits,
-// where a value next to a tie rounds the other way) the accumulator is handed over every 16 MMAs (g.hand = kSegment) and
-// added up by the epilogue warps in registers, rounding to nearest.  bf16 results are handed over every 128 MMAs
-// (kCoarseHand, 4096 of the contraction): what that loses stays below 2^-16 of the sum of magnitudes, and products of up to
-// 4096 keep one accumulator per tile (every 64 MMAs cost 307 -> 318 us on 4 nodes 4096x4096x4096).  Results in 8 bits from tiles
-// of 128 columns are handed over every 8 MMAs (kFineHand), which brings their sums from 1.06-1.25 times the error of plain
-// fp32 sums to 0.96-1.20 (32 nodes 32x784x1024 over six seeds) and costs 39.0 -> 40.5 us there, 473.6 -> 480.8 us on 112 nodes
-// 64x2048x2048, three accumulators in turn (40.9 and 484 us with two).  A tile of 256 columns has one accumulator and waits
-// at each hand-over (weights and product of 4 nodes 4096x4096x4096: 411 us every 16 MMAs, 521 every 8), so it keeps to 16.
+// where a value next to a tie rounds the other way) the accumulator is handed over every 16 MMAs (kSegment) or, for 8 bits,
+// every 8 (kFineHand), and added up by the epilogue warps in registers, rounding to nearest.  bf16 results are handed over
+// every 128 MMAs (kCoarseHand, 4096 of the contraction): what that loses stays below 2^-16 of the sum of magnitudes, and
+// products of up to 4096 keep one accumulator per tile (every 64 MMAs cost 307 -> 318 us on 4 nodes 4096x4096x4096).
+// 8 MMAs instead of 16 bring the sums behind a checkpoint from 1.06-1.25 times the error of plain fp32 sums to 0.96-1.20 (32
+// nodes 32x784x1024 over six seeds) and cost 39.0 -> 40.5 us there, 473.6 -> 480.8 us on 112 nodes 64x2048x2048, three
+// accumulators in turn (40.9 and 484 us with two).  256 columns leave room for one accumulator beside the scales, which waits
+// at each hand-over (weights and product of 4 nodes 4096x4096x4096: 411 us every 16 MMAs, 521 every 8), so they are for bf16.
 // The epilogue takes an accumulator into registers and frees it before it does anything else, so that even a single
 // 256-column one (two leave no room for the scales) keeps the tensor core waiting for a few hundred cycles only.  The
 // registers come from the other warps (setmaxnreg).
@@ -110,7 +110,7 @@ template <int MODE, int BN, bool PAIR> struct Shape {
     static __device__ __forceinline__ uint32_t acc_col(uint32_t i) {
         return i * (uint32_t)BN + (ACCS == 3 && i == 2 ? kScaleCol + kScaleSets * kScaleSet - 2 * (uint32_t)BN : 0u);
     }
-    static constexpr uint32_t MAXIMA = MODE == kForward && COLS == 64 ? 2048 : 0;   // [tile parity][half][128 rows]
+    static constexpr uint32_t MAXIMA = MODE == kForward && BN == 128 ? 2048 : 0;   // [tile parity][half][128 rows]
     // alignment, output staging, barriers
     static constexpr uint32_t OUT = MODE == kWeight ? 0 : kStageOut;                // output staging of a warp
     static constexpr uint32_t FIXED = 1024 + kEpiWarps * OUT + MAXIMA + 1024;
@@ -118,10 +118,9 @@ template <int MODE, int BN, bool PAIR> struct Shape {
     static constexpr int THREADS = 32 * (FIRST_EPI + kEpiWarps);
     // registers per thread: launched with 65536 / THREADS rounded down to a multiple of 8 (128 or 168); the first
     // FIRST_EPI warps give theirs to the epilogue: 256 * 88 + 256 * 168 = 256 * 72 + 256 * 184 = 512 * 128,
-    // 128 * 80 + 256 * 208 < 384 * 168.  With 72 / 184 the scale warps spill, but for kInput of 128 columns (the pair of 256
-    // columns 138 bytes of stores and 628 of loads: 302 us for the forward of 4 nodes 4096x4096x4096; with 88 / 168 16 and 184:
-    // 297 us); with 96 / 160 the epilogue of 256 columns does.  kInput of 128 columns is level or better with 72 / 184 (backward
-    // of 32 nodes 32x784x1024: 36.1 against 36.6 us).
+    // 128 * 80 + 256 * 208 < 384 * 168.  With 72 / 184 the scale warps spill, but for kInput of 128 columns (302 us for the
+    // forward of 4 nodes 4096x4096x4096, 297 with 88 / 168); with 96 / 160 the epilogue of 256 columns does.  kInput of 128
+    // columns is level or better with 72 / 184 (backward of 32 nodes 32x784x1024: 36.1 against 36.6 us).
     static constexpr int REGS_FEW = !SCALED ? 80 : MODE == kInput && BN == 128 ? 72 : 88, REGS_EPI = SCALED ? 256 - REGS_FEW : 208;
 };
 
@@ -596,7 +595,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
             } else if (g.out) {
                 uint8_t* dst = g.out + (int64_t)node * g.out_node + (int64_t)m0 * g.out_pitch + (int64_t)n0 * g.out_size;
                 const int bytes = (g.N - n0) * g.out_size;
-                if (g.out_size == 4) {
+                if (BN < 256 && g.out_size == 4) {
 #pragma unroll
                     for (int c = 0; c < COLS / 32; ++c) {
                         uint32_t w[32];
@@ -615,27 +614,24 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
                     }
                 }
             }
-            if constexpr (MODE == kForward && BN >= 128) {
+            if constexpr (MODE == kForward && BN == 128) {
                 if (g.q) {
                     // columns beyond the result are 0 in the padding, also in rows that hold a NaN
                     if (n0 + COLS > g.N) {
 #pragma unroll
                         for (int j = 0; j < COLS; ++j) sum[j] = n0 + j < g.N ? sum[j] : 0.f;
                     }
-                    // the row's block of 128 columns: this thread's own (BN 256), or shared with the warp of the other half
+                    // the row's block of 128 columns, shared with the warp of the other half.  Two buffers: a warp writes one
+                    // again only after its partner has arrived for the tile between, hence has read it
                     uint32_t top = 0;
 #pragma unroll
                     for (int j = 0; j < COLS; ++j) top = max(top, f8::magnitude(sum[j]));
-                    if constexpr (COLS == 64) {
-                        // two buffers: a warp writes one again only after its partner has arrived for the tile between,
-                        // hence has read it
-                        uint32_t* mx = maxima + (tile_i & 1u) * 256 + quad * 32 + lane;
-                        mx[half * 128] = top;
-                        mbar_arrive(max_full + quad);
-                        const bool go = mbar_wait(max_full + quad, tile_i & 1u);
-                        if (!__all_sync(0xffffffffu, go)) { ok = false; break; }
-                        top = max(top, mx[(half ^ 1) * 128]);
-                    }
+                    uint32_t* mx = maxima + (tile_i & 1u) * 256 + quad * 32 + lane;
+                    mx[half * 128] = top;
+                    mbar_arrive(max_full + quad);
+                    const bool go = mbar_wait(max_full + quad, tile_i & 1u);
+                    if (!__all_sync(0xffffffffu, go)) { ok = false; break; }
+                    top = max(top, mx[(half ^ 1) * 128]);
                     const uint32_t ex = f8::scale_byte(top);
                     constexpr int W = COLS / 4;
                     uint32_t w[W];
@@ -644,7 +640,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
                         w[j] = f8::encode_block4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3], ex);
                     const int64_t row0 = (int64_t)node * g.M + m0;
                     store_rows<W>(w, st, g.q + row0 * g.q_pitch + n0, g.q_pitch, rows, (int)g.q_pitch - n0, true, 1, lane);
-                    if (lane < rows && (COLS == 128 || half == 0) && n0 < g.N) {
+                    if (lane < rows && half == 0 && n0 < g.N) {
                         uint8_t* pe = g.qe + (row0 + lane) * g.qe_pitch;
                         const int blk = n0 / f8::kBlock;
                         pe[blk] = (uint8_t)ex;

@@ -25,9 +25,11 @@ struct Operands {
     int64_t a_pitch, b_pitch;
 };
 
-// fine: the result is rounded to 8 bits.  precise: to fp32, or fine (see fp8_gemm.cuh for how often sums are handed over).
+// What the result is rounded to, which decides how often sums are handed over (see fp8_gemm.cuh).
+enum Rounding { kTo8, kToBf16, kToF32 };
+
 template <int MODE, int BN, bool PAIR>
-cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool fine = false) {
+cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, Rounding to) {
     using S = Shape<MODE, BN, PAIR>;
     auto kernel = fp8_gemm_kernel<MODE, BN, PAIR>;
     const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
@@ -53,7 +55,8 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool f
     if (!ok) return cudaErrorInvalidValue;
     const uint32_t stage_bytes = g.block_bytes * S::KPS;
     g.stages = std::min<int>(kMaxStages, (int)((kSmemLimit - S::FIXED) / stage_bytes));
-    g.hand = !precise ? kCoarseHand : fine && S::ACCS > 1 ? kFineHand : kSegment;
+    if (BN == 256 && S::SCALED && to != kToBf16) return cudaErrorInvalidValue;      // their epilogue rounds to bf16 only
+    g.hand = to == kToBf16 ? kCoarseHand : to == kTo8 ? kFineHand : kSegment;
     g.m_tiles = (g.M + S::TM - 1) / S::TM;
     g.n_tiles = (g.N + BN - 1) / BN;
     const int64_t total = (int64_t)c->n * g.m_tiles * g.n_tiles;
@@ -68,23 +71,53 @@ cudaError_t launch(dpsgd_ctx* c, const Operands& o, Args g, bool precise, bool f
                                    S::FIXED + g.stages * stage_bytes, c->stream, mapA, mapB, g);
 }
 
-// Up to 128 rows per node the product streams the weights, and tiles of 128 columns, whose three accumulators overlap the
-// epilogue with the next tile, are level with wider ones or better.  With more rows it is bound by what the operands bring
-// from L2 (about 64 bytes per cycle and SM): pairs of CTAs share a tile of 256 rows and 256 columns, 32 KB per CTA and
-// k-block instead of 48 for 128 rows and 256 columns, unless such tiles leave far more SMs idle in the last round (training
-// forward of 4 nodes 4096x4096x4096: 293 us, 312 from single CTAs of 256 columns, 393 of 128).  kInput keeps to single CTAs of
-// 256 columns (the backward of those nodes: level within the noise, 816-844 us either way).
-template <int MODE>
-cudaError_t launch_wide(dpsgd_ctx* c, const Operands& o, const Args& g, bool precise, bool fine = false) {
-    const int64_t sms = sm_count(c);
-    const auto cost = [&](int rows, int cols) {                     // rounds over the SMs, times columns per CTA
-        const int64_t tiles = (int64_t)c->n * ((g.M + rows - 1) / rows) * ((g.N + cols - 1) / cols) * (rows / kTileM);
-        return (tiles + sms - 1) / sms * cols;
-    };
-    constexpr bool PAIR = MODE == kForward;
-    if (g.M > kTileM && cost(PAIR ? 2 * kTileM : kTileM, 256) <= cost(128, 128) * 1.3) return launch<MODE, 256, PAIR>(c, o, g, precise, fine);
-    return launch<MODE, 128, false>(c, o, g, precise, fine);
+int64_t rounds(int64_t tiles, int64_t places) { return (tiles + places - 1) / places; }
+
+// Tiles of the forward product by the time they are expected to take, in us: rounds over the SMs (over pairs of them for the
+// pair), times what a tile costs by itself (more where rows of the result are not aligned to 16 bytes and leave element by
+// element) and per k-block.  The costs are a fit to 1634 random shapes (1 to 112 nodes, 1 to 4096 rows, widths of 128 to
+// 4096) and choose a tile within 0.4 % of the best one on average, 26 % at worst.  Narrow tiles give every SM one when there are
+// few rows; a pair (bf16 results only: its one accumulator waits at each hand-over, which others need every 8 or 16 MMAs)
+// reads 32 KB per k-block and SM where single CTAs of 256 columns read 48 (an SM takes about 64 bytes per cycle from L2):
+// training forward of 4 nodes 4096x4096x4096 293 us, 312 from single CTAs of 256 columns, 393 of 128.  With fp32 results and
+// checkpoints 128 columns are level with the pair at best and up to 1.5 times as fast (32 nodes 400x2048x1003 fp32: 55 against
+// 84 us; 16 nodes 512x2048x2048 with a checkpoint 55 against 61).
+struct TileCost { int rows, cols; double once, tile, odd_tile, block; };
+constexpr TileCost kTiles[] = {{128, 32, 0.0, 0.60, 1.2, 0.155}, {128, 64, 0.0, 0.82, 1.6, 0.18}, {128, 128, 0.0, 1.4, 3.4, 0.28},
+                               {256, 256, 1.4, 2.9, 4.4, 0.34}};
+
+cudaError_t launch_forward(dpsgd_ctx* c, const Operands& o, const Args& g, Rounding to) {
+    const int sms = sm_count(c);
+    int best = 2;                                                   // a checkpoint needs whole blocks of 128 columns in a tile
+    double least = 0.0;
+    for (int i = 0; i < 4 && to != kTo8; ++i) {
+        const TileCost& t = kTiles[i];
+        if (t.rows > kTileM && (g.M <= kTileM || to != kToBf16)) continue;
+        const int64_t tiles = (int64_t)c->n * ((g.M + t.rows - 1) / t.rows) * ((g.N + t.cols - 1) / t.cols);
+        const double each = (g.out_vec ? t.tile : t.odd_tile) + t.block * ((g.K + 127) / 128);
+        const double us = t.once + (double)rounds(tiles, std::max(1, sms / (t.rows / kTileM))) * each;
+        if (i == 0 || us <= least) { least = us; best = i; }
+    }
+    switch (best) {
+        case 0: return launch<kForward, 32, false>(c, o, g, to);
+        case 1: return launch<kForward, 64, false>(c, o, g, to);
+        case 2: return launch<kForward, 128, false>(c, o, g, to);
+        default: return launch<kForward, 256, true>(c, o, g, to);
+    }
 }
+
+// dx: 256 columns for bf16 results with more than 128 rows, unless such tiles leave far more SMs idle in the last round.  1.2 to
+// 1.3 as a limit is within 0.1 % of the better one of the two over 135 random shapes (always 128: 1.8 %).  With fp32 results
+// 128 columns stay within 0.3 % (143 shapes; one accumulator, as above).
+cudaError_t launch_input(dpsgd_ctx* c, const Operands& o, const Args& g, Rounding to) {
+    const auto cost = [&](int cols) {
+        return rounds((int64_t)c->n * ((g.M + kTileM - 1) / kTileM) * ((g.N + cols - 1) / cols), sm_count(c)) * cols;
+    };
+    if (to == kToBf16 && g.M > kTileM && cost(256) <= cost(128) * 1.3) return launch<kInput, 256, false>(c, o, g, to);
+    return launch<kInput, 128, false>(c, o, g, to);
+}
+
+Rounding rounding(int dtype) { return dtype == DPSGD_F32 ? kToF32 : kToBf16; }
 
 void set_out(Args& g, void* out, int dtype, int rows, int cols) {
     const int size = dtype == DPSGD_F32 ? 4 : 2;
@@ -153,15 +186,7 @@ cudaError_t launch_fp8_forward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* x
     g.q = yq; g.q_pitch = f8::q_pitch(O); g.qe = ye; g.qe_pitch = f8::e_pitch(O);
     g.bias = bias; g.bias_node = c->ld; g.relu = relu;
     const Operands o{xq, wq, f8::q_pitch(K), f8::q_pitch(K)};
-    const int64_t rows = (int64_t)c->n * ((B + kTileM - 1) / kTileM);
-    const auto tiles = [&](int bn) { return rows * ((O + bn - 1) / bn); };
-    const bool precise = yq || dtype == DPSGD_F32;
-    // A checkpoint needs whole blocks of 128 columns in a tile.  Otherwise, few rows take narrower tiles so that every SM
-    // has one; a tile costs about as much as 64 more columns before its first MMA (7 nodes 77x1001x1003: two rounds of 32
-    // columns 19.4 us, one of 64 columns 18.4 us).
-    if (yq || tiles(128) >= sm_count(c)) return launch_wide<kForward>(c, o, g, precise, yq != nullptr);
-    const auto cost = [&](int bn) { return (tiles(bn) + sm_count(c) - 1) / sm_count(c) * (bn + 64); };
-    return cost(64) <= cost(32) ? launch<kForward, 64, false>(c, o, g, precise) : launch<kForward, 32, false>(c, o, g, precise);
+    return launch_forward(c, o, g, yq ? kTo8 : rounding(dtype));
 }
 
 cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* xe, const uint8_t* wq, const uint8_t* we,
@@ -190,7 +215,7 @@ cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* 
     // (512 MiB) 107 / 109, 40 137 / 133, 112 434 / 372; 128 samples on these 471 / 429, 192 486 / 501, 256 448 / 525; 1024
     // samples on 64 nodes 674 / 691; 4096 samples of 4096x4096 on 4 nodes 478 / 500.
     const bool stream = K > kTileM && B <= kPairSamples && (double)c->n * K * O * 4.0 >= 512.0 * 1024 * 1024;
-    e = stream ? launch<kWeight, 256, true>(c, w, g, true) : launch<kWeight, 256, false>(c, w, g, true);
+    e = stream ? launch<kWeight, 256, true>(c, w, g, kToF32) : launch<kWeight, 256, false>(c, w, g, kToF32);
     if (e != cudaSuccess || !dx) return e;
     // dx waits for the weight gradient, although it needs the launch before it only: a kernel may read what it has not itself
     // waited for only at its own risk (33.0 us without the wait against 36.0 on 32 nodes 32x784x1024, 23.9 against 25.3 on 7
@@ -200,7 +225,7 @@ cudaError_t launch_fp8_backward(dpsgd_ctx* c, const uint8_t* xq, const uint8_t* 
     h.ae = de; h.ae_pitch = f8::e_pitch(O);
     h.we = we; h.we_pitch = f8::e_pitch(K); h.we_node = h.we_pitch * ((O + f8::kBlock - 1) / f8::kBlock);
     set_out(h, dx, dx_dtype, B, K);
-    return launch_wide<kInput>(c, Operands{dq, wq, f8::q_pitch(O), f8::q_pitch(K)}, h, dx_dtype == DPSGD_F32);
+    return launch_input(c, Operands{dq, wq, f8::q_pitch(O), f8::q_pitch(K)}, h, rounding(dx_dtype));
 }
 
 }  // namespace dpsgd

@@ -6,7 +6,7 @@ import torch
 from oracle import fp8_oracle as fo
 from paper_1705_09056_b200 import binding, workloads as wl
 from tests.gpu_util import GpuRun
-from tests.test_gpu_fp8_layers import TOL_SUM, Layer
+from tests.test_gpu_fp8_layers import PAIRS, SHAPES, TOL_BF16, TOL_SUM, Layer
 
 pytestmark = pytest.mark.gpu
 
@@ -157,3 +157,17 @@ def test_weight_gradient_beyond_l2_on_both_sides_of_the_sample_limit(B):
         got = G[i, :N].view(O, K).cpu().numpy().astype(np.float64)
         assert (np.abs(got - d8.T @ xv) <= TOL_SUM * (np.abs(d8).T @ np.abs(xv))).all()
     ctx.close()
+
+
+# bf16 results alone choose among four tiles; the last three are shared by pairs of CTAs, ragged in every direction and with
+# two tiles per pair
+@pytest.mark.parametrize("n,B,K,O", SHAPES + PAIRS + [(24, 256, 2100, 768), (18, 1000, 1100, 500), (9, 257, 4097, 1025)])
+def test_forward_with_a_bf16_result_alone(n, B, K, O):
+    l = Layer(n, B, K, O, off=3)
+    y = l.ctx.fp8_linear_forward(l.x8, l.w8, b_off=l.b_off, relu=True, dtype=torch.bfloat16).float().cpu().numpy().astype(np.float64)
+    ref, scale = l.forward(True)
+    assert (np.abs(y - ref) <= TOL_SUM * scale + TOL_BF16 * np.abs(ref)).all()
+    y2 = torch.full((n, B, O), 7.0, dtype=torch.bfloat16, device="cuda")
+    l.ctx.fp8_linear_forward(l.x8, l.w8, b_off=l.b_off, relu=True, out=y2)
+    assert np.array_equal(y2.float().cpu().numpy().astype(np.float64), y)                # reproducible
+    l.close()
