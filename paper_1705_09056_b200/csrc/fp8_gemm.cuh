@@ -39,9 +39,9 @@
 // The epilogue takes an accumulator into registers and frees it before it does anything else, so that even a single
 // 256-column one (two leave no room for the scales) keeps the tensor core waiting for a few hundred cycles only.  The
 // registers come from the other warps (setmaxnreg).
-// Measured: forward with a checkpoint out, 112 nodes 64 x 2048 x 2048: 99 us, 4.7 TB/s of 8-bit weights (the last round of
+// Measured: forward with a checkpoint out, 112 nodes 64 x 2048 x 2048: 95 us, 4.9 TB/s of 8-bit weights (the last round of
 // tiles is a tenth full; 92 us with 16 MMAs per accumulator); backward of the same layer without dx: 434 us from single CTAs,
-// 372 from pairs, 5.1 TB/s of stores, held back by its operand loads; forward, 4 nodes 4096 x 4096 x 4096: 208 us, 2.6 PFLOP/s.
+// 370 from pairs, 5.1 TB/s of stores, held back by its operand loads; forward, 4 nodes 4096 x 4096 x 4096: 201 us, 2.7 PFLOP/s.
 // Every mbarrier wait is bounded; one that runs out raises the status word, the TMA thread waits (bounded) for its loads
 // in flight and the CTA frees its tensor memory before it returns.
 #pragma once
