@@ -336,6 +336,7 @@ DPSGD_API dpsgd_status dpsgd_ckpt8_load(dpsgd_ctx* ctx, const uint8_t* q_dev, co
 /*
  * 8-bit form of every node's weight block (d_out x d_in, row-major, first column w_off of the parameter row) of the
  * CURRENT X: what dpsgd_fp8_linear_forward and _backward multiply with.  Call it again after X has changed.
+ * For other parameters (the average of the nodes, say) use a context of one node that is bound to them.
  */
 DPSGD_API dpsgd_status dpsgd_fp8_weights(dpsgd_ctx* ctx, int64_t w_off, int32_t d_out, int32_t d_in, uint8_t* wq_dev,
                                          uint8_t* we_dev);

@@ -370,7 +370,8 @@ class Dpsgd:
         return out
 
     def fp8_weights(self, w_off: int, d_out: int, d_in: int, out: Optional[Fp8Weights] = None) -> Fp8Weights:
-        """8-bit form of every node's d_out x d_in weight block at column w_off of the current X."""
+        """8-bit form of every node's d_out x d_in weight block at column w_off of the current X (for other parameters, such
+        as the average of the nodes: a context of one node bound to them)."""
         if out is None:
             out = self.fp8_weights_empty(d_out, d_in)
         assert out.n == self.n and out.d_out == d_out and out.d_in == d_in
